@@ -11,10 +11,15 @@
 //   S^T = K Q^T     [128 keys x rows]   A: K, a key in a lane, D / 2 columns
 //   O^T += V^T P^T  [D x rows]          A: V, a channel in a lane, 64 columns
 // with Q and P, which are small, on the right in shared memory.  Both operands
-// are f16: n s / 16 is exact in it, the queries are scaled by a power of two to
-// the top of its range (exact down to 2^-24 of the largest; the scores are scaled
-// back in 32 bits), and P is rounded to it, 2^-11 of each weight where O is rounded to
-// 2^-8 at the end.  Sums, maxima, statistics and O are in 32 bits.
+// are f16: n s / 16 is exact in it, the queries are scaled by a power of two to the top of
+// its range and the scores back in 32 bits, and P is rounded to it, 2^-11 of each weight where
+// O is rounded to 2^-8 at the end.  A work's rows have one power of two where their largest
+// values are within 2^8 of each other (a row is then off by 2^-30 of its largest value at
+// most, against 2^-23 of each sum), and else each its own, so that no row's result depends
+// on another's size: their scores are then rescaled where they lie, in a copy of the
+// softmax, which a pass over like rows does not run (looking which it is costs 1 to 2%; with a
+// scale of its own for every row of every work 24 branches took 348 us against 308).  Sums,
+// maxima, statistics and O are in 32 bits.
 //
 // A block (one an SM, 20 warps) takes work after work, a work being a run of pages
 // (or a prefill tile) of one KV head and layer for up to 64 rows.  Its stages of
@@ -69,6 +74,7 @@ constexpr uint32_t kTmemK = 0, kTmemV = 128, kTmemS = 256, kTmemO = 384;  // 64 
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kUnset = -1e30f;      // a row's reference before it has seen a key
 constexpr float kHeadroom = 15.f, kBelow = 8.f;
+constexpr int kAlike = 8;             // powers of two between rows that have one scale
 constexpr int kMaxDevices = 64;
 // Registers a thread: what the block is launched with is shared out anew among its
 // five warpgroups (the softmax has a sum, and up to 64 rows a score, of each row in
@@ -111,7 +117,8 @@ struct Meta {
   int32_t red[2][4][kKv4Rows];
   int64_t row[2][2 * kKv4Rows];   // row of Q (layer, row, head), -1 beyond the work's
   int32_t seen[2][2 * kKv4Rows];  // prefill: keys of the run that the row sees
-  float scale[2];             // of the scores, log2 domain
+  float own[2][2 * kKv4Rows];     // unlike rows: a row's own share of the scale, negative
+  float scale[2];             // of the scores, log2 domain; negative where the rows are unlike
   uint32_t tmem;
   uint64_t bars[52];
 };
@@ -662,6 +669,10 @@ struct Kernel {
         return reinterpret_cast<uint4*>(to + (other ? C::kQTile : 0) + (c >> 3) * kKv4Rows * 128 + r * 128 +
                                         (((c & 7) ^ (r & 7)) << 4));
       };
+      auto own_at = [&](int i) {  // and its row's place in meta.own
+        const int x = (i * 32 + lane) / kChunks;
+        return kWide && x >= cols ? x - cols + kKv4Rows : x;
+      };
       // All in flight at once, and in short loops, since a block's first queries are loaded
       // by code that it has not run (133 rows onto 23041: 115.6 -> 111.6 us; by eights through registers before).
       const int mine = (kWide ? 2 : 1) * cols * kChunks / 32;  // a multiple of 4
@@ -672,26 +683,61 @@ struct Kernel {
         copy16_async(place(i), p.q + (row >= 0 ? row * D + lane % kChunks * 8 : 0), row >= 0);
       }
       copies_wait();
-      uint32_t top = 0;  // the largest finite magnitude, as bf16 bits, of each half
-#pragma unroll 2
-      for (int i = 0; i < mine; ++i) {
-        const uint4 v = *place(i);
+      // The largest finite magnitude of 16 bytes, as bf16 bits.
+      auto top_of = [](const uint4& v) -> uint32_t {
         const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+        uint32_t two = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t a = x[e] & 0x7fff7fffu;
-          top = __vmaxu2(top, a & ~__vcmpgeu2(a, 0x7f807f80u));
+          two = __vmaxu2(two, a & ~__vcmpgeu2(a, 0x7f807f80u));
         }
+        return max(two & 0xffffu, two >> 16);
+      };
+      auto unlike_by = [](uint32_t most, uint32_t least) { return (int)(most >> 7) - (int)(least >> 7) > kAlike; };
+      // Of all rows the most, and (zeros aside) the least: of any 16 bytes first, since no row's is below that.
+      uint32_t most = 0, least = 0xffffffffu;
+#pragma unroll 2
+      for (int i = 0; i < mine; ++i) {
+        const uint32_t top = top_of(*place(i));
+        most = max(most, top);
+        least = min(least, top - 1u);
       }
-      top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
+      most = __reduce_max_sync(0xffffffffu, most);
+      bool unlike = most > 0 && unlike_by(most, __reduce_min_sync(0xffffffffu, least) + 1u);
+      if (unlike) {  // each row's own
+        least = 0xffffffffu;
+#pragma unroll 1
+        for (int i = 0; i < mine; ++i) {
+          uint32_t top = top_of(*place(i));
+#pragma unroll
+          for (int h = 1; h < kChunks; h *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, h));
+          least = min(least, top - 1u);
+          if (lane % kChunks == 0) meta.own[b][own_at(i)] = __uint_as_float(top);
+        }
+        unlike = unlike_by(most, __reduce_min_sync(0xffffffffu, least) + 1u);
+      }
       // by 2^e the largest comes to [2^13, 2^14)
-      const int e = min(100, 140 - (int)max(top >> 7, 1u));
-      const float by = __uint_as_float((uint32_t)(e + 127) << 23);
-      if (lane == 0) meta.scale[b] = p.scale_log2 * 16.f * __uint_as_float((uint32_t)(127 - e) << 23);
+      auto power = [](uint32_t top) { return min(100, 140 - (int)max(top >> 7, 1u)); };
+      auto two_to = [](int e) { return __uint_as_float((uint32_t)(e + 127) << 23); };
+      const int all = unlike ? 0 : power(most);
+      if (lane == 0) {
+        const float x = p.scale_log2 * 16.f * two_to(-all);
+        meta.scale[b] = unlike ? -x : x;
+      }
+      __syncwarp();
 #pragma unroll 2
       for (int i = 0; i < mine; ++i) {
         const uint4 v = *place(i);
         const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+        int e = all;
+        if (unlike) {
+          float* own = &meta.own[b][own_at(i)];
+          e = power(__float_as_uint(*own));
+          __syncwarp();
+          if (lane % kChunks == 0) *own = -two_to(-e);
+        }
+        const float by = two_to(e);
         uint32_t y[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -708,7 +754,7 @@ struct Kernel {
   // ---- softmax --------------------------------------------------------------------------
   // A group's stages of a work, for up to kCols rows (g0 stages before it in the
   // block), and half of its results.  False when a wait of any warp ran out.
-  template <int kCols>
+  template <int kCols, bool kUnlike = false>
   __device__ __forceinline__ bool softmax(const Work& k, int n, int g0, int group, int warp, int lane) {
     const int key = warp * 32 + lane, qb = n & 1, stages = stages_of(k), id = 1 + group;
     const uint32_t mine = tmem + ((uint32_t)(warp * 32) << 16);
@@ -737,6 +783,19 @@ struct Kernel {
       bool masks;
       if constexpr (kCausal) masks = (t + 1) * kKv4Keys > seen[0];  // the first row sees the fewest
       else masks = (t + 1) * kKv4Keys > k.n_keys;
+      if constexpr (kUnlike) {  // each row's scores by its own share of the scale, where they lie
+        const float* own = meta.own[qb] + r0;
+#pragma unroll 1
+        for (int j = 0; j < kCols; j += 8) {
+          float y[8];
+          tmem_ld8(s_at + j, y);
+          uint32_t u[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(y[i] * own[j + i]);
+          tmem_st8u_nowait(s_at + j, u);
+        }
+        tmem_wait_st();
+      }
       float s[kCols];  // over the rows' references, keys that a row does not see hidden
       // A second time where a reference has moved (the scores are computed in one place,
       // since another would need as many registers again), and no third.
@@ -855,7 +914,7 @@ struct Kernel {
         meta.sum[group][key] = (__int_as_float(red[0][key]) + __int_as_float(red[1][key])) +
                                 (__int_as_float(red[2][key]) + __int_as_float(red[3][key]));
     }
-    const int64_t scale = kCausal && k.split < 0 ? D : (int64_t)p.max_splits * D;
+    const int64_t stride = kCausal && k.split < 0 ? D : (int64_t)p.max_splits * D;
     float* part = p.part_o + (int64_t)k.split * D + key;
     const int64_t* rows = meta.row[qb] + r0;
     auto put_lse = [&](int i, float m, float sum) {  // 0: the row sees none of these keys
@@ -866,8 +925,8 @@ struct Kernel {
       else p.part_lse[row * p.max_splits + k.split] = lse;
     };
     auto put_o = [&](int64_t row, float y) {
-      if (kCausal && k.split < 0) p.o[row * scale + key] = __float2bfloat16_rn(y);
-      else part[row * scale] = y;
+      if (kCausal && k.split < 0) p.o[row * stride + key] = __float2bfloat16_rn(y);
+      else part[row * stride] = y;
     };
     const int g1 = g0 + stages - 1;
     if constexpr (kWide) {
@@ -954,7 +1013,12 @@ struct Kernel {
       const Work k = work_at(w);
       // eights of rows: what the products have beyond them counts for nothing
       const int rows = kWide ? min(cols_of(k), k.n_rows - stream * cols_of(k)) : k.n_rows;
-      if (rows <= 16) ok = softmax<16>(k, n, g, stream, warp, lane);
+      // unlike rows, of any number, in a copy that scales each by itself
+      const bool there = wait(&q_full[n & 1], n >> 1 & 1);
+      timeout(there, lane);
+      if (there && *reinterpret_cast<volatile float*>(&meta.scale[n & 1]) < 0.f)
+        ok = softmax<64, true>(k, n, g, stream, warp, lane);
+      else if (rows <= 16) ok = softmax<16>(k, n, g, stream, warp, lane);
       else if (rows <= 24) ok = softmax<24>(k, n, g, stream, warp, lane);
       else if (rows <= 32) ok = softmax<32>(k, n, g, stream, warp, lane);
       else if (rows <= 40) ok = softmax<40>(k, n, g, stream, warp, lane);
