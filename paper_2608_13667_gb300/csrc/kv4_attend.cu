@@ -36,7 +36,8 @@
 //           a stage, a score of each row.  The reference of a row is 8 (log2)
 //           below the maximum when it was last set, and set anew only when a score
 //           comes 15 above it, 7 above that maximum (f16 holds 2^16): then the
-//           group finds the new maximum and rescales its O and sums.  Sums stay
+//           group finds the new maximum and rescales its O and sums.  Scores so large that
+//           fp32 has them off by more than that count as at most 15 above.  Sums stay
 //           per key until the work's end, where a narrow work's two streams are joined.
 //   8..15   unpacking, a group for every other stage: thread t unpacks key t of K, then
 //           channel t of V (a group's 32 channels are one warp's, so that a token's
@@ -72,8 +73,9 @@ constexpr int kPages = kKv4Keys / kPageTokens;  // of a stage
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kTmemK = 0, kTmemV = 128, kTmemS = 256, kTmemO = 384;  // 64 columns for each of two
 constexpr float kLn2 = 0.69314718055994530942f;
-constexpr float kUnset = -1e30f;      // a row's reference before it has seen a key
+constexpr float kUnset = -1e30f;      // a row's reference before it has seen a key: finite, any will do
 constexpr float kHeadroom = 15.f, kBelow = 8.f;
+constexpr float kOff = 0x1p-21f;      // of a score and its reference: eight roundings
 constexpr int kAlike = 8;             // powers of two between rows that have one scale
 constexpr int kMaxDevices = 64;
 // Registers a thread: what the block is launched with is shared out anew among its
@@ -819,8 +821,13 @@ struct Kernel {
 #pragma unroll
         for (int i = 2; i + 3 < kCols; i += 4) a = fmax3(a, s[i], s[i + 1]), b = fmax3(b, s[i + 2], s[i + 3]);
         const float highest = fmax3(a, b, fmaxf(s[kCols - 2], s[kCols - 1]));
-        if (!any_of<128>(id, first || !ok || (highest > kHeadroom && !moved))) break;
+        if (!any_of<128>(id, first || !ok || highest > kHeadroom)) break;
         if (any_of<128>(id, !ok)) return fails();
+        if (moved) {  // scores of 10^7 and more, which fp32 has off by as much: these keys alike
+#pragma unroll
+          for (int i = 0; i < kCols; ++i) s[i] = s[i] > kHeadroom ? kHeadroom : s[i];
+          break;
+        }
 #pragma unroll 1
         for (int j = 0; j < kCols; j += 8) {
           float y[8];
@@ -839,8 +846,11 @@ struct Kernel {
           int o = max(max(red[0][key], red[1][key]), max(red[2][key], red[3][key]));
           o ^= o >> 31 & 0x7fffffff;
           const float top = __int_as_float(o), old = first ? kUnset : -ref[key];
-          const bool moves = top - old > kHeadroom;
-          const float m = moves ? top - kBelow : old;
+          // Below the maximum by what fp32 may have it off as well, and never lower than it was
+          // (a NaN stays one).
+          const float to = top - kBelow - fabsf(top) * kOff;
+          const bool moves = first ? top != -INFINITY : top - old > kHeadroom && !(to < old);
+          const float m = moves ? to : old;
           ref[key] = -m;
           factor[key] = moves ? ex2(old - m) : 1.f;
         }
@@ -891,7 +901,7 @@ struct Kernel {
     // ---- the work's results: sums over the keys, O of both groups out of tensor memory
     if (any_of<128>(id, !ok)) return fails();
     if (first) {  // the group has had none of its stages
-      if (key < kCols) meta.sum[group][key] = 0.f, ref[key] = -kUnset;
+      if (key < kCols) meta.sum[group][key] = 0.f;
     } else {
 #pragma unroll
       for (int j = 0; j < kCols; j += 16) {
@@ -971,7 +981,8 @@ struct Kernel {
     const int c0 = group * kHalf, mine_n = group ? kCols - kHalf : kHalf;
     if (key < mine_n) {
       const int i = c0 + key;
-      const float ma = -meta.m[0][i], mb = -meta.m[1][i], m = fmaxf(ma, mb);
+      const float ma = meta.sum[0][i] == 0.f ? -INFINITY : -meta.m[0][i];
+      const float mb = meta.sum[1][i] == 0.f ? -INFINITY : -meta.m[1][i], m = fmaxf(ma, mb);
       const float fa = meta.sum[0][i] == 0.f ? 0.f : ex2(ma - m), fb = meta.sum[1][i] == 0.f ? 0.f : ex2(mb - m);
       const float sum = fa * meta.sum[0][i] + fb * meta.sum[1][i];
       const float over = sum == 0.f ? 0.f : 16.f / sum;
