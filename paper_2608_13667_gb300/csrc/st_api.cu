@@ -1570,7 +1570,7 @@ st_status decode_impl(st_pool* P, const std::vector<int>& slots, const void* q, 
     aw.item_base = 0;
     aw.beside_prev = n_wide + n_pair > 0 ? 1 : 0;
     return launch_decode_tc(P->kmap, P->vmap, aw, ip, n_narrow, c.head_dim, false, s);
-  }, (n_narrow > 0 ? 1 : 0) + (n_wide > 0 ? 1 : 0) + (n_pair > 0 ? 1 : 0),
+  }, is_kv4(c) ? 1 : (n_narrow > 0 ? 1 : 0) + (n_wide > 0 ? 1 : 0) + (n_pair > 0 ? 1 : 0),
                   dp.reread_bytes + part_bytes);
   if (st != ST_OK) {
     if (ps >= 0) retire_plan(P, ps, s);  // its copy may still be in flight
