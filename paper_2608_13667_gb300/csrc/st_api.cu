@@ -531,6 +531,8 @@ st_status kv4_append_small(st_pool* P, const int* slots, const std::vector<Appen
   Plan plan;
   int ps = -1;
   st_status st = ST_OK;
+  double overhead = 0;  // the copied rows read and written, and the table entries
+  for (const CowEvent& c : cows) overhead += c.rows * token_bytes(P->cfg) * P->cfg.n_layers * 2;
   if (dirty.runs > 0) {
     st = acquire_plan(P, &plan, &ps);
     if (st != ST_OK) return st;
@@ -540,9 +542,10 @@ st_status kv4_append_small(st_pool* P, const int* slots, const std::vector<Appen
     p.values = t.values;
     p.table_out = P->d_tables;
     p.n_table_blocks = t.n_runs;
+    overhead += (double)t.n_values * 8 + t.n_runs * 16;
   }
   st = run_kernel(P, kKAppend, kv4_row_bytes(P->cfg) * n_rows, 0, s,
-                  [&] { return launch_kv4_append(p, &inl, P->cfg.head_dim, s); }, 1, kv4_copy_bytes(P->cfg, cows.size()));
+                  [&] { return launch_kv4_append(p, &inl, P->cfg.head_dim, s); }, 1, overhead);
   const st_status rs = ps >= 0 ? retire_plan(P, ps, s) : ST_OK;
   return st == ST_OK ? rs : st;
 }

@@ -29,3 +29,19 @@ def test_a_decode_is_one_launch_and_its_combine(stlib, branches):
     pool.decode_attn(br, zeros(2, len(br), 16, 128))
     got = pool.profile_read()
     assert got["decode_partial"]["kernels"] == 1 and got["lse_combine"]["kernels"] == 1
+
+
+def test_a_small_append_counts_its_tables_and_copied_rows(stlib):
+    pool = make(stlib)
+    token = 2 * 2 * 136 * 2  # layers, KV heads, K and V
+    m = pool.seq_create()
+    pool.profile_read()
+    pool.append_kv([m], zeros(2, 1, 165, 2, 128), zeros(2, 1, 165, 2, 128))
+    got = pool.profile_read()["append_kv"]
+    assert got["kernels"] == 1 and got["overhead_bytes"] == 11 * 8 + 16  # 11 entries, one range
+    pool.append_kv([m], zeros(2, 1, 3, 2, 128), zeros(2, 1, 3, 2, 128))
+    assert pool.profile_read()["append_kv"]["overhead_bytes"] == 0
+    f, = pool.fork(m, 1)
+    pool.append_kv([f], zeros(2, 1, 1, 2, 128), zeros(2, 1, 1, 2, 128))
+    got = pool.profile_read()["append_kv"]  # the table of a fork goes out whole; 8 rows of its last page copied
+    assert got["kernels"] == 1 and got["overhead_bytes"] == 8 * token * 2 + 11 * 8 + 16
