@@ -87,6 +87,7 @@ typedef int64_t st_seq;
  *    library's own (a page spans every KV head of a layer, 17 * head_dim / 2 bytes a head);
  *  - O comes out in bf16, the queries' type: a cache that is off by a tenth
  *    has no use for more.  The log-sum-exp stays fp32.
+ *  - a sequence has at most 2^31 - 256 rows: an append beyond fails with ST_ERR_OOM;
  *  - st_decode_attn_noalloc refuses the flag. */
 #define ST_FLAG_KV4 4
 typedef struct st_pool st_pool;

@@ -93,6 +93,10 @@ __device__ __forceinline__ uint32_t kv4_word(const uint32_t* n) {
   return w - bias * (0x4b400000u + kKv4Zero - 8) + (five << 30 | five >> 2);
 }
 
+// Rows of a sequence at most: their numbers are 32 bits wide here, up to the end of the
+// last stage of keys.  (A bf16 pool's memory ends before that.)
+constexpr int64_t kKv4MostRows = INT32_MAX - 255;
+
 // ---- append, copy, read back (kv4_store.cu) --------------------------------------
 
 struct Kv4Branch {

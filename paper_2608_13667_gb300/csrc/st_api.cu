@@ -595,6 +595,9 @@ st_status do_append_rows(st_pool* P, const int* slots, const int32_t* counts, in
   for (int i = 0; i < n_br; ++i) {
     if (!bp.fits(slots[i], counts[i]))
       return fail(P, ST_ERR_OOM, "sequence would exceed max_pages (%d)", bp.max_pages());
+    if (is_kv4(P->cfg) && bp.slot(slots[i]).len + counts[i] > kKv4MostRows)
+      return fail(P, ST_ERR_OOM, "sequence would exceed the %lld rows that a 4-bit pool's may have",
+                  (long long)kKv4MostRows);
     need += bp.pages_needed(slots[i], counts[i]);
     n_rows += counts[i];
     uniform = uniform && counts[i] == counts[0];
