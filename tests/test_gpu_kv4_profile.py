@@ -33,7 +33,7 @@ def test_a_decode_is_one_launch_and_its_combine(stlib, branches):
 
 def test_a_small_append_counts_its_tables_and_copied_rows(stlib):
     pool = make(stlib)
-    token = 2 * 2 * 136 * 2  # layers, KV heads, K and V
+    token = 2 * 2 * 2 * (1088 // 16)  # layers, KV heads, K and V
     m = pool.seq_create()
     pool.profile_read()
     pool.append_kv([m], zeros(2, 1, 165, 2, 128), zeros(2, 1, 165, 2, 128))
