@@ -106,9 +106,6 @@ struct Kv4Branch {
   int32_t n;      // rows
   int32_t page0;  // pages of the branches before it
 };
-struct Kv4InlineBranches {
-  Kv4Branch b[kInlineAppendBranches];
-};
 struct Kv4StoreParams {
   const __nv_bfloat16* k;  // [L][n_rows][Hkv][D]
   const __nv_bfloat16* v;
@@ -138,8 +135,8 @@ struct Kv4InlineAppend {
 constexpr int kKv4TableBlocks = 32;  // most of a small append
 
 cudaError_t launch_kv4_append(const Kv4StoreParams& p, const Kv4InlineAppend* inl, int D, cudaStream_t s);
-// Rows read back, from a 4-bit pool or (kv4 false) a bf16 one.
-cudaError_t launch_read_kv(const Kv4StoreParams& p, const Kv4InlineBranches* inl, bool kv4, int D, cudaStream_t s);
+// Rows of one branch read back, from a 4-bit pool or (kv4 false) a bf16 one.
+cudaError_t launch_read_kv(const Kv4StoreParams& p, const Kv4Branch& rows, bool kv4, int D, cudaStream_t s);
 
 struct Kv4InlineCows {
   CowCopy c[kInlineCows];

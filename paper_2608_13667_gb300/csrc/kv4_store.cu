@@ -202,14 +202,13 @@ __global__ void __launch_bounds__(2 * D) kv4_append_kernel(const Kv4StoreParams 
 
 // Rows read back: a page as above; kKv4 false: of a bf16 pool.
 template <int D, bool kKv4>
-__global__ void __launch_bounds__(2 * D) read_kernel(const Kv4StoreParams p,
-                                                     const __grid_constant__ Kv4InlineBranches inl) {
+__global__ void __launch_bounds__(2 * D) read_kernel(const Kv4StoreParams p, const __grid_constant__ Kv4Branch rows) {
   constexpr int kLanes = D / 8;
   constexpr int kPageBytes = kKv4 ? kv4_page_bytes(D) : kPageTokens * D * 2;
   griddep_wait();
   griddep_launch_dependents();
   const int layer = blockIdx.z;
-  const PageOfCall pg = page_of_call(p, p.branches ? p.branches : inl.b, blockIdx.x);
+  const PageOfCall pg = page_of_call(p, &rows, blockIdx.x);
   if ((uint64_t)pg.block >= (uint64_t)p.n_blocks) {
     if (threadIdx.x == 0) atomicCAS(p.status, 0, kDevBadIndex);
     return;
@@ -308,17 +307,15 @@ cudaError_t launch_kv4_append(const Kv4StoreParams& p, const Kv4InlineAppend* in
   return cudaErrorInvalidValue;
 }
 
-cudaError_t launch_read_kv(const Kv4StoreParams& p, const Kv4InlineBranches* inl, bool kv4, int D, cudaStream_t s) {
-  static const Kv4InlineBranches kNone{};
-  const Kv4InlineBranches& ip = inl ? *inl : kNone;
+cudaError_t launch_read_kv(const Kv4StoreParams& p, const Kv4Branch& rows, bool kv4, int D, cudaStream_t s) {
   if (p.n_pages == 0) return cudaSuccess;
   const dim3 grid(p.n_pages, blocks_of_heads(p), p.L);
   if (D == 128)
-    return kv4 ? launch_chained(read_kernel<128, true>, grid, dim3(256), 0, s, p, ip)
-               : launch_chained(read_kernel<128, false>, grid, dim3(256), 0, s, p, ip);
+    return kv4 ? launch_chained(read_kernel<128, true>, grid, dim3(256), 0, s, p, rows)
+               : launch_chained(read_kernel<128, false>, grid, dim3(256), 0, s, p, rows);
   if (D == 64)
-    return kv4 ? launch_chained(read_kernel<64, true>, grid, dim3(128), 0, s, p, ip)
-               : launch_chained(read_kernel<64, false>, grid, dim3(128), 0, s, p, ip);
+    return kv4 ? launch_chained(read_kernel<64, true>, grid, dim3(128), 0, s, p, rows)
+               : launch_chained(read_kernel<64, false>, grid, dim3(128), 0, s, p, rows);
   return cudaErrorInvalidValue;
 }
 

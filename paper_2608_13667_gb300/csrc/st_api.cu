@@ -1872,9 +1872,7 @@ ST_API st_status st_read_kv(st_pool* P, st_seq seq, int64_t start, int n_tok, vo
   st_status st = flush_tables(P, dirty_tables(*P->pool), s);
   if (st != ST_OK) return poison(P, st);
   Kv4StoreParams p{};
-  Kv4InlineBranches inl;
-  const AppendBranch rows{slot, (int32_t)start, 0, n_tok};
-  inl.b[0] = Kv4Branch{slot, (int32_t)start, 0, n_tok, 0};
+  const Kv4Branch rows{slot, (int32_t)start, 0, n_tok, 0};
   p.k_out = static_cast<__nv_bfloat16*>(k);
   p.v_out = static_cast<__nv_bfloat16*>(v);
   p.k_pool = reinterpret_cast<uint8_t*>(P->k_pool);
@@ -1884,12 +1882,12 @@ ST_API st_status st_read_kv(st_pool* P, st_seq seq, int64_t start, int n_tok, vo
   p.n_blocks = c.n_blocks;
   p.n_br = 1;
   p.n_rows = n_tok;
-  p.n_pages = pages_of_rows(rows);
+  p.n_pages = pages_of_rows(AppendBranch{slot, (int32_t)start, 0, n_tok});
   p.L = c.n_layers;
   p.Hkv = c.n_kv_heads;
   p.max_pages = c.max_pages;
   const double bytes = (double)n_tok * c.n_layers * (token_bytes(c) + c.n_kv_heads * c.head_dim * 4.0);
-  return run_kernel(P, kKRead, bytes, 0, s, [&] { return launch_read_kv(p, &inl, is_kv4(c), c.head_dim, s); });
+  return run_kernel(P, kKRead, bytes, 0, s, [&] { return launch_read_kv(p, rows, is_kv4(c), c.head_dim, s); });
 }
 
 ST_API st_status st_block_table(st_pool* P, st_seq seq, int32_t* out, int cap, int* n_pages,
