@@ -638,10 +638,16 @@ struct Kernel {
     constexpr int kChunks = D / 8;  // of 16 bytes in a row
     int n = 0;
     bool ok = true;
+    int ahead[2] = {0, 0};  // stages of the works whose queries a buffer has
     for (int w = blockIdx.x; w < n_works; w = after(w, n++)) {
       const int b = n & 1;
-      if (!(ok = wait(&q_empty[b], (n >> 1 & 1) ^ 1))) break;
+      // the one wait for a whole work, which may take longer than a wait's limit: another for each 2^18 stages
+      const int waits = 1 + (ahead[b] >> 18);
+      ok = false;
+      for (int i = 0; i < waits && !ok; ++i) ok = wait(&q_empty[b], (n >> 1 & 1) ^ 1);
+      if (!ok) break;
       const Work k = work_at(w);
+      ahead[b] = stages_of(k);
       const int cols = cols_of(k);
       auto row_of = [&](int r) -> int64_t {
         int64_t row;
