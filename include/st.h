@@ -88,6 +88,9 @@ typedef int64_t st_seq;
  *  - O comes out in bf16, the queries' type: a cache that is off by a tenth
  *    has no use for more.  The log-sum-exp stays fp32.
  *  - a sequence has at most 2^31 - 256 rows: an append beyond fails with ST_ERR_OOM;
+ *  - captured into a CUDA graph, st_decode_attn replays as long as its branches stay
+ *    as they are, where its plan fits the kernels' parameters and no block table
+ *    has changed since the last call; else it returns ST_ERR_STATE, as the calls that append do;
  *  - st_decode_attn_noalloc refuses the flag. */
 #define ST_FLAG_KV4 4
 typedef struct st_pool st_pool;
@@ -260,7 +263,8 @@ ST_API st_status st_prefill_batch(st_pool* pool, const st_seq* seqs, int n_seq, 
  * another pool: values read from a 4-bit pool append to one unchanged, but for
  * groups with a scale below 2^-14, which may lose a little again.
  * k, v: device bf16 [n_layers][n_tok][n_kv_heads][head_dim].
- * 0 <= start, start + n_tok <= the sequence's length; n_tok = 0 is a no-op. */
+ * 0 <= start, start + n_tok <= the sequence's length; n_tok = 0 is a no-op.
+ * Not captured into a CUDA graph while block tables have changed (ST_ERR_STATE). */
 ST_API st_status st_read_kv(st_pool* pool, st_seq seq, int64_t start, int n_tok, void* k, void* v,
                             void* stream);
 

@@ -329,6 +329,14 @@ st_status acquire_plan(st_pool* P, Plan* plan, int* slot_out) {
   return ST_OK;
 }
 
+// A graph would read a staging slot again when it is replayed, after other calls have
+// written it, and would repeat a change of the pool that was made once.
+st_status refuse_capture(st_pool* P, cudaStream_t s, const char* what) {
+  cudaStreamCaptureStatus c = cudaStreamCaptureStatusNone;
+  CUDA_TRY(P, cudaStreamIsCapturing(s, &c));
+  return c == cudaStreamCaptureStatusNone ? ST_OK : fail(P, ST_ERR_STATE, "%s cannot be captured into a graph", what);
+}
+
 // The device's address of a place in the pinned staging ring.
 template <class T>
 const T* on_device(st_pool* P, const T* h) {
@@ -588,6 +596,10 @@ st_status kv4_append(st_pool* P, const std::vector<AppendBranch>& brs, const std
 st_status do_append_rows(st_pool* P, const int* slots, const int32_t* counts, int n_br, const void* k,
                          const void* v, cudaStream_t s, bool* deferred = nullptr) {
   if (deferred) *deferred = false;
+  if (is_kv4(P->cfg) && !P->meta_only) {
+    const st_status st = refuse_capture(P, s, "a call that appends to a 4-bit pool");
+    if (st != ST_OK) return st;
+  }
   BlockPool& bp = *P->pool;
   int64_t need = 0, n_rows = 0;
   int cow_bound = 0;  // branches whose append may start with a copy-on-write
@@ -1437,7 +1449,8 @@ st_status kv4_append_and_prefill(st_pool* P, const Kv4Rows* seqs, int n_seq, int
     return fail(P, ST_ERR_INVALID, "prefill of %lld row tiles does not fit one plan slot", (long long)n_tiles);
   Plan plan;
   int ps = -1;
-  st_status st = acquire_plan(P, &plan, &ps);
+  st_status st = refuse_capture(P, s, "a prefill of a 4-bit pool");
+  if (st == ST_OK) st = acquire_plan(P, &plan, &ps);
   if (st != ST_OK) return st;
   std::vector<int> slots(n_seq);
   std::vector<int32_t> counts(n_seq);
@@ -1487,8 +1500,14 @@ st_status decode_impl(st_pool* P, const std::vector<int>& slots, const void* q, 
   if (!inline_plan && plan_bytes({items.size() * sizeof(AttnItem), members.size() * sizeof(int32_t),
                                   n_br * sizeof(int32_t)}) > kStageSlotBytes)
     return fail(P, ST_ERR_INVALID, "decode plan of %d items does not fit one plan slot", (int)items.size());
+  const DirtyTables dirty = dirty_tables(*P->pool);
+  st_status st = ST_OK;
+  if (is_kv4(c) && (!inline_plan || dirty.runs > 0)) {
+    st = refuse_capture(P, s, inline_plan ? "the refresh of changed block tables" : "a decode plan this large");
+    if (st != ST_OK) return st;
+  }
   // device tables that missed an upload would disagree with the host's
-  st_status st = flush_tables(P, dirty_tables(*P->pool), s);
+  st = flush_tables(P, dirty, s);
   if (st != ST_OK) return poison(P, st);
 
   InlineDecodePlan inl;
@@ -1869,7 +1888,10 @@ ST_API st_status st_read_kv(st_pool* P, st_seq seq, int64_t start, int n_tok, vo
   if (c.n_layers > kMaxGridLayers) return fail(P, ST_ERR_INVALID, "rows of more than %d layers", kMaxGridLayers);
   DeviceGuard guard(P->device);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  st_status st = flush_tables(P, dirty_tables(*P->pool), s);
+  const DirtyTables dirty = dirty_tables(*P->pool);
+  st_status st = dirty.runs > 0 ? refuse_capture(P, s, "the refresh of changed block tables") : ST_OK;
+  if (st != ST_OK) return st;
+  st = flush_tables(P, dirty, s);
   if (st != ST_OK) return poison(P, st);
   Kv4StoreParams p{};
   const Kv4Branch rows{slot, (int32_t)start, 0, n_tok, 0};
