@@ -85,8 +85,11 @@ typedef int64_t st_seq;
  * held (a merge's or a step's own new rows among them), with these differences:
  *  - k_pool and v_pool are st_kv_bytes(cfg) bytes each, in a layout of the
  *    library's own (a page spans every KV head of a layer, 17 * head_dim / 2 bytes a head);
- *  - O comes out in bf16, the queries' type: a cache that is off by a tenth
- *    has no use for more.  The log-sum-exp stays fp32.
+ *  - O comes out in bf16, the queries' type, and its weights are rounded to f16 (2^-11
+ *    of each) before they are summed in fp32: a cache that is off by a tenth
+ *    has no use for more.  The log-sum-exp is of the unrounded weights and stays fp32;
+ *  - a decode step appends in a launch of its own, and prefills take longer (2048 rows
+ *    onto 16896, four layers: a third longer);
  *  - a sequence has at most 2^31 - 256 rows: an append beyond fails with ST_ERR_OOM;
  *  - captured into a CUDA graph, st_decode_attn replays as long as its branches stay
  *    as they are, where its plan fits the kernels' parameters and no block table
@@ -191,7 +194,7 @@ ST_API st_status st_decode_attn(st_pool* pool, const st_seq* br, int n_br, const
  * n_tok = 1 followed by st_decode_attn on the same branches, in fewer
  * launches: the decode kernel that reads a branch's last page writes the new
  * row into it first.  (When a branch's last page is shared and partly filled,
- * the step copies it with a separate append launch first.)
+ * or the pool has ST_FLAG_KV4, a separate append launch goes first.)
  * k, v: device bf16 [n_layers][n_br][n_kv_heads][head_dim], the new rows;
  * q, o, lse: as st_decode_attn.  Branches may be empty before the call.
  * Failures before the append change nothing; a failure after it (a CUDA
@@ -215,7 +218,9 @@ ST_API st_status st_decode_step(st_pool* pool, const st_seq* br, int n_br, const
  *           (M = 128) tile, for 65 to 128 stacked rows, bit 2: the paired
  *           tile (two M = 128 tiles of one CTA, for 129 to 256 stacked rows);
  *           neither: the narrow tile, up to 64 stacked rows.  Narrow items
- *           come first, then wide, then paired.
+ *           come first, then wide, then paired.  A 4-bit pool has no paired tile
+ *           (larger groups are cut into wide ones), its items come longest
+ *           first, and a CTA takes them one after another, one CTA an SM.
  * members:  int32 [member_cap]
  * n_splits: int32 [n_br], partial results per branch (each split index
  *           0 .. n_splits - 1 is written by exactly one item)

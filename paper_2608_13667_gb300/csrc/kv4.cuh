@@ -180,7 +180,7 @@ struct Kv4AttnParams {
   int32_t n_items, n_rows_q, Hq, Hkv, G, L, max_pages, max_splits;
   int32_t hold_loads;       // test hook (ST_FLAG_HOLD_LOADS)
   int32_t wide;             // works of up to 128 rows
-  int32_t keep_l2;          // the launch's pages fit in L2: loaded to stay there
+  int32_t keep_l2;          // pages are loaded to stay in L2: a decode's that fit there, a prefill's, which several row tiles read
 };
 
 cudaError_t launch_kv4_attend(const Kv4AttnParams& p, const InlineDecodePlan* inl, int D, cudaStream_t s);

@@ -30,8 +30,9 @@
 // A wide work has up to 128 rows: those of a group beyond 64, and of a prefill.  Each softmax
 // group then takes every stage, for half of the rows, and the two share a stage's K and
 // V, which lie in the stages' two places in turn.  What is unpacked once serves twice the
-// rows: 24 branches of 8 heads over 65536 tokens, two groups and layers, 396 -> 364 us (278 with
-// longer runs and rows by eights); 2048 rows of 32/8 heads onto 16896, four layers, 3340 -> 2650.  Roles:
+// rows: 24 branches of 8 heads over 65536 tokens, two groups and layers, 396 -> 364 us (315 since, with
+// longer runs and rows by eights); 2048 rows of 32/8 heads onto 16896, four layers, 3340 -> 2980 (2810
+// since, with registers shared out for it).  Roles:
 //   0..7    softmax, two groups of 128 threads: thread t has key t of
 //           a stage, a score of each row.  The reference of a row is 8 (log2)
 //           below the maximum when it was last set, and set anew only when a score
@@ -53,9 +54,13 @@
 //
 // What bounds it: the latencies of these roles.  A stage of 40 rows takes a block 1500 cycles (131072
 // tokens of 5 branches, four agents and layers: 3.2 TB/s of pages), one of 128 rows 2500;
-// the tensor core is busy for some 400 and 1700 of them, the exponentials take 400 and 1000 of
+// the tensor core is busy for some 400 and 1050 of them, the exponentials take 320 and 1000 of
 // their pipe, instructions go out in half of the cycles, and the loads would come at
-// 5.6 TB/s.
+// 5.6 TB/s.  The unpacking groups have the least slack: a stream's stage takes 3400 cycles, its
+// K and V some 3070 of their group, a softmax group's part 2230.
+//
+// How far sums reach: the tensor core cuts off each step of O's, so over equal weights of one
+// sign O is low by 1e-4 of itself at 2^20 keys a run, 2e-3 at 2^22, 8e-3 at 2^23.
 #include <math.h>
 
 #include <mutex>
@@ -84,8 +89,8 @@ constexpr int kMaxDevices = 64;
 // have, so a build that launches with fewer is refused.
 constexpr int kLaunchRegs = 96;
 // A wide prefill's groups have 64 rows each as a rule, and with 144 registers wait for what
-// they spilled (four layers, 2048 rows onto 16896: 3.10 ms against 2.65; with 152 2.95, with
-// 168 2.74); a decode's have fewer, and unpacking with 56 costs it 8% (24 branches).
+// they spilled (four layers, 2048 rows onto 16896, in a short run: 2.98 ms against 2.56 with 160;
+// with 152 2.99, with 168 2.74); a decode's have fewer, and unpacking with 56 costs it 8% (24 branches).
 template <bool kCausal, bool kWide>
 struct Regs {
   static constexpr bool kMore = kCausal && kWide;

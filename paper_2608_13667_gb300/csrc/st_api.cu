@@ -1038,10 +1038,10 @@ namespace {
 constexpr int64_t kKv4WorkStages = 4;
 
 // Pages of a run in a 4-bit pool's decode: blocks that stay (one an SM) take run after
-// run, and of the lengths tried (whole stages, each some half longer than the one before) the one
+// run, and of the lengths tried (whole stages: each up to six, then each a sixth longer than the one before) the one
 // after which the last block ends first is taken.  One layer, 8 heads, us with runs of 1, 5 and 16
-// stages: 8192 tokens of 5 branches 29.0, 23.8 and 30.1; 16 such agents of
-// 4k to 32k with runs of 10, 32 and 64: 161, 138 and 155.
+// stages and as planned: 8192 tokens of 5 branches 27.3, 22.2, 28.3 and 21.2; 16 such agents of
+// 4k to 32k with runs of 10, 32 and 64 and as planned: 153, 136, 130 and 131 (events around the call, L2 flushed).
 int64_t kv4_chunk(const DecodePlan& d, int n_br, int prefix_most, int64_t heads, int64_t sms) {
   constexpr int64_t kStage = kKv4Keys / kPageTokens;
   auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
@@ -1364,8 +1364,9 @@ st_status kv4_prefill(st_pool* P, const Kv4Rows* seqs, int n_seq, int32_t R, con
     longest = std::max<int64_t>(longest, (int64_t)seqs[i].L0 + seqs[i].T);
   }
   // The split after which the last block ends first, where it gains three hundredths (the partial
-  // results have to be written and read): 512 works of 181 stages, 4 rounds of 152 blocks, take 852 us
-  // in halves and 886 whole.
+  // results have to be written and read): 512 works of 181 stages, 4 rounds of 152 blocks, take 853 us
+  // in halves, 880 whole and 910 in thirds.  All works count alike: 40 of 181 stages, four of five with 128 rows
+  // and one with 20, take 122 us as split here and 115 in thirds.
   const int64_t works = n_rows_tiles * c.n_kv_heads * c.n_layers, stages_most = (longest + kKv4Keys - 1) / kKv4Keys;
   const int64_t rows_all = (int64_t)R * c.n_q_heads * c.n_layers, room = (int64_t)partial_rows(c);
   int want = 1;
@@ -1575,6 +1576,9 @@ st_status decode_impl(st_pool* P, const std::vector<int>& slots, const void* q, 
       kp.n_items = n_items;
       kp.max_splits = c.max_splits;
       kp.keep_l2 = ap.keep_l2;
+      // One wide group makes the call's launch wide.  Us, against a launch for each height: 24 branches
+      // over 16384 beside eight groups of 5, two layers, 236 and 264; 12 over 4096 beside sixteen of 5, one
+      // layer, 84 and 133; with narrow runs of the group's own rows alone, 138 and 174.
       for (const AttnItem& it : items) kp.wide |= it.flags & kItemWide ? 1 : 0;
       return launch_kv4_attend(kp, ip, c.head_dim, s);
     }
