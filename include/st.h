@@ -299,7 +299,8 @@ ST_API st_status st_harvest(const int32_t* streams, int stride, const int32_t* l
 /* Queries and keys from a layer's projections: each head of a row is normed by
  * its root mean square, x / sqrt(mean x^2 + eps) * w, and its first rotary_dim
  * dimensions are rotated by the row's position, pair i by the angle pos * f_i.
- * All in fp32, rounded once to the bf16 that the other calls take.
+ * All in fp32 (a normed head of values beyond 10^18, whose squares are not, comes out as
+ * zeros), rounded once to the bf16 that the other calls take.
  * q, k:   device, of `type`: head h of row r of layer l begins at element
  *         l * layer_stride + r * row_stride + h * head_dim, so that views of a
  *         fused projection need no copy.  16-byte aligned, as the strides are.
